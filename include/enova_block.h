@@ -15,7 +15,9 @@
  * throws; arguments are checked on the host before any launch, and a failing call writes no output;
  * pointers are device memory unless they are said to be the host's; calls are asynchronous on `stream`,
  * those on one handle must not overlap, and a handle's workspace grows on demand (a growing call waits
- * for the device, and is refused while `stream` is being captured into a graph). Matrices are row-major
+ * for the device, and is refused while `stream` is being captured into a graph). A graph that captured
+ * calls holds the workspace that they were given: a handle keeps it when a later call needs a larger one,
+ * has to outlive the graph, and a replay counts as a call on it. Matrices are row-major
  * with the row pitch ("ld", in elements) given where one is; `rows` may be 0. Types: ENOVA_F32 or
  * ENOVA_BF16 for a handle's matrices; sums and norms are formed in 32 bits. Buffers of one call must not
  * overlap unless it is said that they may.

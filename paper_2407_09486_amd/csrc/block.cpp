@@ -50,23 +50,43 @@ int few_rows(bool packed, int64_t weight_bytes)
 constexpr int kWidest = 262144;
 constexpr int64_t kMostRows = int64_t{1} << 30;
 
-// A handle's device workspace: grows on demand, and is handed out in 256-byte aligned pieces.
+// A handle's device workspace: grows on demand, and is handed out in 256-byte aligned pieces. Launches that a graph
+// captured hold its address, so a buffer that a captured call was given stays allocated until the handle goes.
 struct Workspace {
     char *p = nullptr;
     size_t cap = 0;
+    bool captured = false;             // by a call that was given p
+    std::vector<char *> outgrown;
 
-    ~Workspace() { (void)hipFree(p); }
+    ~Workspace()
+    {
+        (void)hipFree(p);
+        for (char *q : outgrown)
+            (void)hipFree(q);
+    }
     enova_status need(size_t bytes, hipStream_t stream)
     {
-        if (bytes <= cap)
-            return ENOVA_OK;
         hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
-        (void)hipStreamIsCapturing(stream, &capturing);
+        if (hipStreamIsCapturing(stream, &capturing) != hipSuccess)
+            (void)hipGetLastError();
+        if (bytes <= cap) {
+            captured |= capturing != hipStreamCaptureStatusNone;
+            return ENOVA_OK;
+        }
         if (capturing != hipStreamCaptureStatusNone)
             return fail(ENOVA_EINVAL, "the workspace has to grow to %zu bytes, which a stream under capture cannot: make one such call before", bytes);
-        (void)hipFree(p);              // waits for the work that uses it
+        if (captured) {
+            try {
+                outgrown.push_back(p);
+            } catch (const std::bad_alloc &) {
+                return fail(ENOVA_ENOMEM, "host memory");
+            }
+        } else {
+            (void)hipFree(p);          // waits for the work that uses it
+        }
         p = nullptr;
         cap = 0;
+        captured = false;
         const hipError_t e = hipMalloc(reinterpret_cast<void **>(&p), bytes);
         if (e != hipSuccess) {
             p = nullptr;
