@@ -4,9 +4,14 @@ Each class owns one library handle; its methods check and marshal their argument
 entry points on torch's current stream (or the one given). All computation happens in the
 library's HIP kernels. Matrices are two-dimensional, in the handle's type, with neighbouring
 columns next to each other in memory; where a method says so, rows may be further apart.
+
+A method that is given a stream works there as torch's own operations do under ``torch.cuda.stream``: what
+it returns is allocated on that stream, and the caller orders the stream after the work that makes the
+arguments, and keeps them until the work is done.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import numpy as np
@@ -49,6 +54,14 @@ def _dense(t, dtype, shape, what):
     return t.data_ptr()
 
 
+_CURRENT = contextlib.nullcontext()
+
+
+def _on(stream):
+    """Where a call's results are allocated: on the stream that writes them."""
+    return _CURRENT if stream is None else torch.cuda.stream(stream)
+
+
 class _Handle:
     handle = None
 
@@ -86,9 +99,10 @@ class GatedBlock(_Handle):
         return (_dense(wg, self.dtype, up, "wg"), _dense(wu, self.dtype, up, "wu"),
                 _dense(wd, self.dtype, (self.model, self.hidden), "wd"))
 
-    def saved(self, rows, device="cuda"):
+    def saved(self, rows, device="cuda", stream=None):
         """A buffer for what forward leaves for backward (g, u and h)."""
-        return torch.empty(self._saved_floats(rows), dtype=torch.float32, device=device)
+        with _on(stream):
+            return torch.empty(self._saved_floats(rows), dtype=torch.float32, device=device)
 
     def _saved_floats(self, rows):
         n = ctypes.c_int64()
@@ -103,10 +117,11 @@ class GatedBlock(_Handle):
         px, ldx = _matrix(x, self.dtype, self.model, "x")
         rows = x.shape[0]
         if y is None:
-            y = torch.empty((rows, self.model), dtype=self.dtype, device=x.device)
+            with _on(stream):
+                y = torch.empty((rows, self.model), dtype=self.dtype, device=x.device)
         py, ldy = _matrix(y, self.dtype, self.model, "y", rows)
         if save and saved is None:
-            saved = self.saved(rows, x.device)
+            saved = self.saved(rows, x.device, stream)
         _check(lib().enova_gated_forward(self.handle, px, ldx, rows, *self._weights(wg, wu, wd), py, ldy,
                                          self._kept(saved, rows), self._queue(stream)), "enova_gated_forward")
         return y if saved is None else (y, saved)
@@ -116,8 +131,9 @@ class GatedBlock(_Handle):
         px, ldx = _matrix(x, self.dtype, self.model, "x")
         rows = x.shape[0]
         pdy, lddy = _matrix(dy, self.dtype, self.model, "dy", rows)
-        dx = torch.empty((rows, self.model), dtype=self.dtype, device=x.device) if input_grad else None
-        dw = [torch.empty_like(w) for w in (wg, wu, wd)] if weight_grads else [None] * 3
+        with _on(stream):
+            dx = torch.empty((rows, self.model), dtype=self.dtype, device=x.device) if input_grad else None
+            dw = [torch.empty_like(w) for w in (wg, wu, wd)] if weight_grads else [None] * 3
         _check(lib().enova_gated_backward(self.handle, px, ldx, rows, *self._weights(wg, wu, wd),
                                           self._kept(saved, rows), pdy, lddy,
                                           None if dx is None else dx.data_ptr(), self.model,
@@ -150,8 +166,9 @@ class ResidualNorm(_Handle):
         """(res, out, stats); stats is for backward."""
         shape = (residual.shape[0], self.model)
         rows = shape[0]
-        res, out = torch.empty_like(residual), torch.empty_like(residual)
-        stats = torch.empty((rows, 4), dtype=torch.float32, device=residual.device)
+        with _on(stream):
+            res, out = torch.empty_like(residual), torch.empty_like(residual)
+            stats = torch.empty((rows, 4), dtype=torch.float32, device=residual.device)
         _check(lib().enova_resnorm_forward(
             self.handle, _dense(residual, self.dtype, shape, "residual"), _dense(branch, self.dtype, shape, "branch"),
             rows, self._vector(post, "post"), self._vector(post_bias, "post_bias"), self._vector(pre, "pre"),
@@ -164,11 +181,12 @@ class ResidualNorm(_Handle):
         "dpre_bias", "dgate" of those that are there."""
         shape = (residual.shape[0], self.model)
         rows, dev = shape[0], residual.device
-        g = {"dr": torch.empty_like(residual), "do": torch.empty_like(residual),
-             "dpre": torch.empty(self.model, dtype=torch.float32, device=dev)}
-        for name, t in (("dpost", post), ("dpost_bias", post_bias), ("dpre_bias", pre_bias), ("dgate", gate)):
-            if t is not None:
-                g[name] = torch.empty_like(t)
+        with _on(stream):
+            g = {"dr": torch.empty_like(residual), "do": torch.empty_like(residual),
+                 "dpre": torch.empty(self.model, dtype=torch.float32, device=dev)}
+            for name, t in (("dpost", post), ("dpost_bias", post_bias), ("dpre_bias", pre_bias), ("dgate", gate)):
+                if t is not None:
+                    g[name] = torch.empty_like(t)
         p = {k: t.data_ptr() for k, t in g.items()}
         _check(lib().enova_resnorm_backward(
             self.handle, _dense(residual, self.dtype, shape, "residual"), _dense(branch, self.dtype, shape, "branch"),
@@ -236,6 +254,9 @@ class AdamW(_Handle):
         p = _flat(grads, (self._grad_type,), "grads", self._sizes)
         _check(lib().enova_adamw_set_grads(self.handle, (ctypes.c_void_p * len(p))(*p), self._queue(stream)),
                "enova_adamw_set_grads")
+        if stream is not None:                 # steps queued there may still read the old ones
+            for t in self.grads:
+                t.record_stream(stream)
         self.grads = list(grads)
 
     def step(self, lr=None, grad_scale=1.0, stream=None):
@@ -249,7 +270,8 @@ class AdamW(_Handle):
         if self.bits == 32 and m is None and v is None:
             return self.m, self.v
         if m is None or v is None:
-            m, v = ([torch.empty_like(p, dtype=torch.float32) for p in self.params] for _ in range(2))
+            with _on(stream):
+                m, v = ([torch.empty_like(p, dtype=torch.float32) for p in self.params] for _ in range(2))
         pm, pv = (_flat(t, (torch.float32,), "states", self._sizes) for t in (m, v))
         n = len(pm)
         _check(lib().enova_adamw_states(self.handle, (ctypes.c_void_p * n)(*pm), (ctypes.c_void_p * n)(*pv),
@@ -287,7 +309,12 @@ class Int8Linear(_Handle):
         """y [rows, outputs]; rows of x and y may be apart."""
         px, ldx = _matrix(x, self.dtype, self.columns, "x")
         if y is None:
-            y = torch.empty((x.shape[0], self.outputs), dtype=self.dtype, device=x.device)
+            with _on(stream):
+                y = torch.empty((x.shape[0], self.outputs), dtype=self.dtype, device=x.device)
         py, ldy = _matrix(y, self.dtype, self.outputs, "y", x.shape[0])
         _check(lib().enova_i8_forward(self.handle, px, ldx, x.shape[0], py, ldy, self._queue(stream)), "enova_i8_forward")
+        if stream is not None:                 # the handle may go before the product is done
+            for t in (self.codes, self.scales, self.bias):
+                if t is not None:
+                    t.record_stream(stream)
         return y

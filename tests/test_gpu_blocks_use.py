@@ -56,3 +56,92 @@ def test_int8_graph_outlives_larger_calls():
     want = op(x[:80])
     for got in replayed(lambda: [op(x[:80])], lambda n: op(x[:2000 * n])):
         assert torch.equal(got[0], want)
+
+
+# ----------------------------------------------------------------------------- streams
+def stream_of(t):
+    """The stream whose memory pool holds a tensor."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not of torch's allocator")
+
+
+def on_both(call):
+    """call(stream)'s tensors on torch's current stream and on one given; the latter have to belong to it."""
+    want = call(None)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = torch.empty(1 << 26, device="cuda")
+    for _ in range(20):
+        busy.normal_()                         # the current stream is behind
+    got = call(side)
+    side.synchronize()
+    assert all(stream_of(t) == side.cuda_stream for t in got)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()
+
+
+def test_block_results_belong_to_the_stream_given():
+    t = block_inputs(700, 256, 384, "bf16", 4)
+    op = blocks.GatedBlock(256, 384)
+
+    def call(stream):
+        y, kept = op.forward(*t[:4], save=True, stream=stream)
+        return [y, kept, *op.backward(*t[:4], t[4], kept, stream=stream), op.saved(300, stream=stream)]
+
+    def without_the_rest(stream):
+        y, kept, *grads = call(stream)[:-1]
+        return [y, *grads]
+
+    on_both(without_the_rest)
+    side = torch.cuda.Stream()
+    assert all(stream_of(a) == side.cuda_stream for a in call(side)[1::5])
+    torch.cuda.synchronize()
+
+
+def test_norm_results_belong_to_the_stream_given():
+    t, d = norm_inputs(300, 1000, "f32", 7, 20)
+    op = blocks.ResidualNorm(1000, dtype="f32", norm="layer", group=20)
+    w = [t[k] for k in ("post", "pre", "post_bias", "pre_bias")]
+
+    def call(stream):
+        res, out, stats = op.forward(t["residual"], t["branch"], *w, gate=t["gate"], stream=stream)
+        g = op.backward(t["residual"], t["branch"], *w, *d, stats, gate=t["gate"], stream=stream)
+        return [res, out, stats, *g.values()]
+
+    on_both(call)
+
+
+def test_int8_and_adamw_results_belong_to_the_stream_given():
+    g = rng(8)
+    codes, scales = blocks.quantize_weight(normal(g, 96, 500).float().cuda())
+    op = blocks.Int8Linear(codes, scales, dtype="f32")
+    for rows in (1, 20, 300):
+        x = normal(g, rows, 500).float().cuda()
+        on_both(lambda stream: [op(x, stream=stream)])
+    p = [normal(g, n).float().cuda() for n in (5000, 300)]
+    adam = blocks.AdamW(p, [a * 0.1 for a in p], bits=8)
+    adam.step()
+    on_both(lambda stream: [a for part in adam.states(stream=stream) for a in part])
+
+
+def test_what_a_handle_drops_waits_for_the_stream_given():
+    """Gradients that set_grads replaces are not reused before the steps queued on the stream are done."""
+    g = rng(9)
+    side = torch.cuda.Stream()
+    p = [normal(g, 1 << 20).float().cuda()]
+    old = normal(g, 1 << 20).float().cuda()
+    at, op = old.data_ptr(), blocks.AdamW(p, [old])
+    fresh = torch.zeros(1 << 20, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        busy = torch.empty(1 << 28, device="cuda")
+        for _ in range(100):
+            busy.normal_()
+    op.step(stream=side)
+    op.set_grads([fresh], stream=side)
+    del old
+    again = torch.empty(1 << 20, device="cuda")
+    assert again.data_ptr() != at
+    torch.cuda.synchronize()
