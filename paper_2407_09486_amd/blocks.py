@@ -181,6 +181,7 @@ class ResidualNorm(_Handle):
         "dpre_bias", "dgate" of those that are there."""
         shape = (residual.shape[0], self.model)
         rows, dev = shape[0], residual.device
+        self._vector(pre_bias, "pre_bias")     # its gradient's shape, and nothing else
         with _on(stream):
             g = {"dr": torch.empty_like(residual), "do": torch.empty_like(residual),
                  "dpre": torch.empty(self.model, dtype=torch.float32, device=dev)}

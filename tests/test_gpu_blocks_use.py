@@ -145,3 +145,20 @@ def test_what_a_handle_drops_waits_for_the_stream_given():
     again = torch.empty(1 << 20, device="cuda")
     assert again.data_ptr() != at
     torch.cuda.synchronize()
+
+
+# ----------------------------------------------------------------------------- refusals
+@pytest.mark.parametrize("name", ["post", "pre", "post_bias", "pre_bias"])
+@pytest.mark.parametrize("bad", ["type", "short", "host", "apart"])
+def test_norm_vectors_are_checked_in_both_directions(name, bad):
+    t, d = norm_inputs(6, 64, "bf16", 3)
+    op = blocks.ResidualNorm(64, norm="layer")
+    order = ("post", "pre", "post_bias", "pre_bias")
+    stats = op.forward(t["residual"], t["branch"], *(t[k] for k in order))[2]
+    torch.cuda.synchronize()
+    v = t[name]
+    t[name] = {"type": v.bfloat16(), "short": v[:63], "host": v.cpu(), "apart": v.repeat_interleave(2)[::2]}[bad]
+    with pytest.raises(ValueError, match=name):
+        op.forward(t["residual"], t["branch"], *(t[k] for k in order))
+    with pytest.raises(ValueError, match=name):
+        op.backward(t["residual"], t["branch"], *(t[k] for k in order), *d, stats)
