@@ -33,27 +33,6 @@ def _known(value, table, what):
     return table[value]
 
 
-def _matrix(t, dtype, cols, what, rows=None):
-    """(pointer, row pitch) of a device matrix whose rows may be apart."""
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows):
-        raise ValueError(f"{what}: expected a device matrix of {cols} columns"
-                         f"{'' if rows is None else f' and {rows} rows'} in {dtype}, got {tuple(t.shape)} {t.dtype}")
-    row, col = t.stride()
-    if (col != 1 and cols > 1) or (row < cols and t.shape[0] > 1):
-        raise ValueError(f"{what}: columns have to be next to each other, and rows must not overlap")
-    return t.data_ptr(), max(row, cols)
-
-
-def _dense(t, dtype, shape, what):
-    """Pointer of a contiguous device tensor (None -> NULL)."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous device tensor of shape {shape} in {dtype}, "
-                         f"got {tuple(t.shape)} {t.dtype}")
-    return t.data_ptr()
-
-
 _CURRENT = contextlib.nullcontext()
 
 
@@ -63,12 +42,46 @@ def _on(stream):
 
 
 class _Handle:
+    """One library handle, on the device that was current when the object was made."""
     handle = None
+
+    def __init__(self):
+        self._device = torch.cuda.current_device()
 
     def _open(self, name, *args):
         h = ctypes.c_void_p()
         _check(getattr(lib(), f"enova_{name}_init")(*args, ctypes.byref(h)), f"enova_{name}_init")
-        self.handle, self._name, self._device = h.value, name, torch.cuda.current_device()
+        self.handle, self._name = h.value, name
+
+    def _matrix(self, t, dtype, cols, what, rows=None):
+        """(pointer, row pitch) of a matrix on the handle's device whose rows may be apart."""
+        if (t.get_device() != self._device or t.dtype != dtype or t.dim() != 2 or t.shape[1] != cols
+                or (rows is not None and t.shape[0] != rows)):
+            raise ValueError(f"{what}: expected a matrix of {cols} columns{'' if rows is None else f' and {rows} rows'} "
+                             f"in {dtype} on cuda:{self._device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+        row, col = t.stride()
+        if (col != 1 and cols > 1) or (row < cols and t.shape[0] > 1):
+            raise ValueError(f"{what}: columns have to be next to each other, and rows must not overlap")
+        return t.data_ptr(), max(row, cols)
+
+    def _dense(self, t, dtype, shape, what):
+        """Pointer of a contiguous tensor on the handle's device (None -> NULL)."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._device or not t.is_contiguous():
+            raise ValueError(f"{what}: expected a contiguous tensor of shape {shape} in {dtype} on cuda:{self._device}, "
+                             f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    def _flat(self, tensors, dtypes, what, sizes):
+        """Their pointers, after a check of a list of contiguous tensors on the handle's device."""
+        if len(tensors) != len(sizes):
+            raise ValueError(f"{what}: {len(tensors)} tensors for {len(sizes)} parameters")
+        for i, t in enumerate(tensors):
+            if t.dtype not in dtypes or t.numel() != sizes[i] or t.get_device() != self._device or not t.is_contiguous():
+                raise ValueError(f"{what}[{i}]: expected a contiguous tensor of {sizes[i]} elements in "
+                                 f"{' or '.join(map(str, dtypes))} on cuda:{self._device}")
+        return [t.data_ptr() for t in tensors]
 
     def _queue(self, stream):
         """The stream given, or torch's current one on the handle's device."""
@@ -91,13 +104,14 @@ class GatedBlock(_Handle):
 
     def __init__(self, model, hidden, dtype="bf16", act="silu"):
         code, self.dtype = _known(dtype, _TYPES, "dtype")
+        super().__init__()
         self.model, self.hidden = model, hidden
         self._open("gated", ctypes.byref(enova_gated_config(model, hidden, code, _known(act, ACTIVATIONS, "activation"))))
 
     def _weights(self, wg, wu, wd):
         up = (self.hidden, self.model)
-        return (_dense(wg, self.dtype, up, "wg"), _dense(wu, self.dtype, up, "wu"),
-                _dense(wd, self.dtype, (self.model, self.hidden), "wd"))
+        return (self._dense(wg, self.dtype, up, "wg"), self._dense(wu, self.dtype, up, "wu"),
+                self._dense(wd, self.dtype, (self.model, self.hidden), "wd"))
 
     def saved(self, rows, device="cuda", stream=None):
         """A buffer for what forward leaves for backward (g, u and h)."""
@@ -110,16 +124,16 @@ class GatedBlock(_Handle):
         return n.value
 
     def _kept(self, saved, rows):
-        return None if saved is None else _dense(saved, torch.float32, (self._saved_floats(rows),), "saved")
+        return None if saved is None else self._dense(saved, torch.float32, (self._saved_floats(rows),), "saved")
 
     def forward(self, x, wg, wu, wd, save=False, y=None, saved=None, stream=None):
         """y, or (y, saved) with ``save`` (or a buffer from ``saved(rows)`` to save in). Rows of x and y may be apart."""
-        px, ldx = _matrix(x, self.dtype, self.model, "x")
+        px, ldx = self._matrix(x, self.dtype, self.model, "x")
         rows = x.shape[0]
         if y is None:
             with _on(stream):
                 y = torch.empty((rows, self.model), dtype=self.dtype, device=x.device)
-        py, ldy = _matrix(y, self.dtype, self.model, "y", rows)
+        py, ldy = self._matrix(y, self.dtype, self.model, "y", rows)
         if save and saved is None:
             saved = self.saved(rows, x.device, stream)
         _check(lib().enova_gated_forward(self.handle, px, ldx, rows, *self._weights(wg, wu, wd), py, ldy,
@@ -128,9 +142,9 @@ class GatedBlock(_Handle):
 
     def backward(self, x, wg, wu, wd, dy, saved=None, input_grad=True, weight_grads=True, stream=None):
         """(dx, dwg, dwu, dwd); None for those not asked for. Without ``saved`` g and u are computed again."""
-        px, ldx = _matrix(x, self.dtype, self.model, "x")
+        px, ldx = self._matrix(x, self.dtype, self.model, "x")
         rows = x.shape[0]
-        pdy, lddy = _matrix(dy, self.dtype, self.model, "dy", rows)
+        pdy, lddy = self._matrix(dy, self.dtype, self.model, "dy", rows)
         with _on(stream):
             dx = torch.empty((rows, self.model), dtype=self.dtype, device=x.device) if input_grad else None
             dw = [torch.empty_like(w) for w in (wg, wu, wd)] if weight_grads else [None] * 3
@@ -150,17 +164,18 @@ class ResidualNorm(_Handle):
 
     def __init__(self, model, dtype="bf16", norm="rms", eps=1e-5, keep=1.0, scale=1.0, group=0):
         code, self.dtype = _known(dtype, _TYPES, "dtype")
+        super().__init__()
         self.model, self.group = model, group
         self._open("resnorm", ctypes.byref(enova_resnorm_config(model, code, _known(norm, NORMS, "norm"), eps, keep,
                                                                 scale, group)))
 
     def _vector(self, t, what):
-        return _dense(t, torch.float32, (self.model,), what)
+        return self._dense(t, torch.float32, (self.model,), what)
 
     def _gate(self, gate, rows):
         if gate is not None and self.group < 1:
             raise ValueError("a gate needs a group of 1 row or more")
-        return None if gate is None else _dense(gate, torch.float32, (-(-rows // self.group), self.model), "gate")
+        return None if gate is None else self._dense(gate, torch.float32, (-(-rows // self.group), self.model), "gate")
 
     def forward(self, residual, branch, post, pre, post_bias=None, pre_bias=None, gate=None, stream=None):
         """(res, out, stats); stats is for backward."""
@@ -170,8 +185,8 @@ class ResidualNorm(_Handle):
             res, out = torch.empty_like(residual), torch.empty_like(residual)
             stats = torch.empty((rows, 4), dtype=torch.float32, device=residual.device)
         _check(lib().enova_resnorm_forward(
-            self.handle, _dense(residual, self.dtype, shape, "residual"), _dense(branch, self.dtype, shape, "branch"),
-            rows, self._vector(post, "post"), self._vector(post_bias, "post_bias"), self._vector(pre, "pre"),
+            self.handle, self._dense(residual, self.dtype, shape, "residual"),
+            self._dense(branch, self.dtype, shape, "branch"), rows, self._vector(post, "post"), self._vector(post_bias, "post_bias"), self._vector(pre, "pre"),
             self._vector(pre_bias, "pre_bias"), self._gate(gate, rows), res.data_ptr(), out.data_ptr(),
             stats.data_ptr(), self._queue(stream)), "enova_resnorm_forward")
         return res, out, stats
@@ -190,24 +205,13 @@ class ResidualNorm(_Handle):
                     g[name] = torch.empty_like(t)
         p = {k: t.data_ptr() for k, t in g.items()}
         _check(lib().enova_resnorm_backward(
-            self.handle, _dense(residual, self.dtype, shape, "residual"), _dense(branch, self.dtype, shape, "branch"),
-            rows, self._vector(post, "post"), self._vector(post_bias, "post_bias"), self._vector(pre, "pre"),
-            self._gate(gate, rows), _dense(stats, torch.float32, (rows, 4), "stats"),
-            _dense(dres, self.dtype, shape, "dres"), _dense(dout, self.dtype, shape, "dout"), p["dr"], p["do"],
+            self.handle, self._dense(residual, self.dtype, shape, "residual"),
+            self._dense(branch, self.dtype, shape, "branch"), rows, self._vector(post, "post"), self._vector(post_bias, "post_bias"), self._vector(pre, "pre"),
+            self._gate(gate, rows), self._dense(stats, torch.float32, (rows, 4), "stats"),
+            self._dense(dres, self.dtype, shape, "dres"), self._dense(dout, self.dtype, shape, "dout"), p["dr"], p["do"],
             p.get("dpost"), p.get("dpost_bias"), p["dpre"], p.get("dpre_bias"), p.get("dgate"), self._queue(stream)),
             "enova_resnorm_backward")
         return g
-
-
-def _flat(tensors, dtypes, what, sizes):
-    """Their pointers, after a check of a list of contiguous device tensors."""
-    if len(tensors) != len(sizes):
-        raise ValueError(f"{what}: {len(tensors)} tensors for {len(sizes)} parameters")
-    for i, t in enumerate(tensors):
-        if t.dtype not in dtypes or t.numel() != sizes[i] or not t.is_cuda or not t.is_contiguous():
-            raise ValueError(f"{what}[{i}]: expected a contiguous device tensor of {sizes[i]} elements in "
-                             f"{' or '.join(map(str, dtypes))}")
-    return [t.data_ptr() for t in tensors]
 
 
 class AdamW(_Handle):
@@ -223,6 +227,7 @@ class AdamW(_Handle):
             raise ValueError("no parameters")
         if bits not in (32, 8):
             raise ValueError(f"states of {bits} bits: 32 or 8")
+        super().__init__()
         dev, sizes = params[0].device, [p.numel() for p in params]
 
         def made(given, dtype, per=1):
@@ -235,14 +240,15 @@ class AdamW(_Handle):
         self.v_scale = made(v_scale, torch.float32, 256) if bits == 8 else None
         self._sizes, self._grad_type = sizes, self.grads[0].dtype if self.grads else torch.float32
         blocks = [-(-n // 256) for n in sizes]
-        lists = [_flat(self.params, (torch.float32,) if params[0].dtype == torch.float32 else (torch.bfloat16,),
+        lists = [self._flat(self.params, (torch.float32,) if params[0].dtype == torch.float32 else (torch.bfloat16,),
                        "params", sizes),
-                 _flat(self.grads, (self._grad_type,) if self._grad_type in _CODES else tuple(_CODES), "grads", sizes),
-                 _flat(self.copies, (torch.bfloat16,), "copies", sizes) if self.copies else [None] * len(sizes),
-                 _flat(self.m, (self.m[0].dtype if m is None else torch.int8 if bits == 8 else torch.float32,), "m", sizes),
-                 _flat(self.v, (torch.uint8 if bits == 8 else torch.float32,), "v", sizes)]
-        lists += ([_flat(self.m_scale, (torch.float32,), "m_scale", blocks),
-                   _flat(self.v_scale, (torch.float32,), "v_scale", blocks)] if bits == 8 else [[None] * len(sizes)] * 2)
+                 self._flat(self.grads, (self._grad_type,) if self._grad_type in _CODES else tuple(_CODES), "grads", sizes),
+                 self._flat(self.copies, (torch.bfloat16,), "copies", sizes) if self.copies else [None] * len(sizes),
+                 self._flat(self.m, (self.m[0].dtype if m is None else torch.int8 if bits == 8 else torch.float32,), "m", sizes),
+                 self._flat(self.v, (torch.uint8 if bits == 8 else torch.float32,), "v", sizes)]
+        lists += ([self._flat(self.m_scale, (torch.float32,), "m_scale", blocks),
+                   self._flat(self.v_scale, (torch.float32,), "v_scale", blocks)]
+                  if bits == 8 else [[None] * len(sizes)] * 2)
         # rows of enova_adamw_tensor: seven pointers and a length
         rows = np.array([[x or 0 for x in row] for row in zip(*lists, sizes)], dtype=np.int64)
         table = rows.ctypes.data_as(ctypes.c_void_p)
@@ -252,7 +258,7 @@ class AdamW(_Handle):
 
     def set_grads(self, grads, stream=None):
         """Other gradient tensors for the steps from here on."""
-        p = _flat(grads, (self._grad_type,), "grads", self._sizes)
+        p = self._flat(grads, (self._grad_type,), "grads", self._sizes)
         _check(lib().enova_adamw_set_grads(self.handle, (ctypes.c_void_p * len(p))(*p), self._queue(stream)),
                "enova_adamw_set_grads")
         if stream is not None:                 # steps queued there may still read the old ones
@@ -273,7 +279,7 @@ class AdamW(_Handle):
         if m is None or v is None:
             with _on(stream):
                 m, v = ([torch.empty_like(p, dtype=torch.float32) for p in self.params] for _ in range(2))
-        pm, pv = (_flat(t, (torch.float32,), "states", self._sizes) for t in (m, v))
+        pm, pv = (self._flat(t, (torch.float32,), "states", self._sizes) for t in (m, v))
         n = len(pm)
         _check(lib().enova_adamw_states(self.handle, (ctypes.c_void_p * n)(*pm), (ctypes.c_void_p * n)(*pv),
                                         self._queue(stream)), "enova_adamw_states")
@@ -297,22 +303,23 @@ class Int8Linear(_Handle):
 
     def __init__(self, codes, scales, bias=None, dtype="bf16", gate=None):
         code, self.dtype = _known(dtype, _TYPES, "dtype")
+        super().__init__()
         self.outputs, self.inputs = codes.shape
-        p, ld = _matrix(codes, torch.int8, self.inputs, "codes")
+        p, ld = self._matrix(codes, torch.int8, self.inputs, "codes")
         self.codes, self.scales, self.bias = codes, scales, bias
         self.columns = self.inputs * (1 if gate is None else 2)
         self._open("i8", ctypes.byref(enova_i8_config(self.inputs, self.outputs, code,
                                                       -1 if gate is None else _known(gate, ACTIVATIONS, "activation"))),
-                   p, ld, _dense(scales, torch.float32, (self.outputs,), "scales"),
-                   _dense(bias, torch.float32, (self.outputs,), "bias"))
+                   p, ld, self._dense(scales, torch.float32, (self.outputs,), "scales"),
+                   self._dense(bias, torch.float32, (self.outputs,), "bias"))
 
     def __call__(self, x, y=None, stream=None):
         """y [rows, outputs]; rows of x and y may be apart."""
-        px, ldx = _matrix(x, self.dtype, self.columns, "x")
+        px, ldx = self._matrix(x, self.dtype, self.columns, "x")
         if y is None:
             with _on(stream):
                 y = torch.empty((x.shape[0], self.outputs), dtype=self.dtype, device=x.device)
-        py, ldy = _matrix(y, self.dtype, self.outputs, "y", x.shape[0])
+        py, ldy = self._matrix(y, self.dtype, self.outputs, "y", x.shape[0])
         _check(lib().enova_i8_forward(self.handle, px, ldx, x.shape[0], py, ldy, self._queue(stream)), "enova_i8_forward")
         if stream is not None:                 # the handle may go before the product is done
             for t in (self.codes, self.scales, self.bias):
