@@ -238,6 +238,10 @@ __global__ void __launch_bounds__(block_threads<TEAM>()) k_resnorm_forward(NormP
         unpack(branch[i], c[i], p.model, whole, o[i]);
         unpack(residual[i], c[i], p.model, whole, r[i]);
     }
+    // In place, a row's last eight values may lie in the piece of another wave's thread as well: nobody stores before all
+    // have read. (With a first norm its sums are that barrier.)
+    if (TEAM > 64 && !p.post && p.res == p.residual)
+        __syncthreads();
     float2 so = make_float2(0.0f, 1.0f);
     if (p.post)
         so = row_stats<TEAM, P>(o, c, p.model, p.layer, p.eps, sum);

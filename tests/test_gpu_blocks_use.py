@@ -5,6 +5,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
+from paper_2407_09486_amd import binding  # noqa: E402
 from test_gpu_blocks import block_inputs, blocks, norm_inputs, normal, rng, run_block, run_norm  # noqa: E402
 
 
@@ -162,3 +163,22 @@ def test_norm_vectors_are_checked_in_both_directions(name, bad):
         op.forward(t["residual"], t["branch"], *(t[k] for k in order))
     with pytest.raises(ValueError, match=name):
         op.backward(t["residual"], t["branch"], *(t[k] for k in order), *d, stats)
+
+
+# ----------------------------------------------------------------------------- in place
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("model", [5, 200, 513, 519, 1030, 2051, 3079, 4095, 6001, 12290])
+def test_norms_in_place(model, dtype, post):
+    """res over residual, at widths whose last piece begins a wave: the row's last values are two threads' to read."""
+    rows = 400
+    t, _ = norm_inputs(rows, model, dtype, model, biases=False, post=post)
+    op = blocks.ResidualNorm(model, dtype=dtype, keep=0.75)
+    want = op.forward(t["residual"], t["branch"], t["post"], t["pre"])
+    res, out, stats = t["residual"].clone(), torch.empty_like(t["residual"]), torch.empty(rows, 4, device="cuda")
+    status = binding.lib().enova_resnorm_forward(
+        op.handle, res.data_ptr(), t["branch"].data_ptr(), rows, t["post"].data_ptr() if post else None, None,
+        t["pre"].data_ptr(), None, None, res.data_ptr(), out.data_ptr(), stats.data_ptr(),
+        torch.cuda.current_stream().cuda_stream)
+    assert status == binding.ENOVA_OK
+    assert all(torch.equal(a, b) for a, b in zip((res, out, stats), want))
