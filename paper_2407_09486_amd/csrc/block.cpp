@@ -788,7 +788,7 @@ enova_status enova_adamw_init(const enova_adamw_config *config, const enova_adam
             return fail(ENOVA_EINVAL, "tensor %d: only fp32 parameters have bf16 copies", i);
         chunks += (t.numel + kAdamChunk - 1) / kAdamChunk;
     }
-    if (chunks > 0x7fffffff)
+    if (chunks * kAdamThreads >= int64_t{1} << 32)         // one launch
         return fail(ENOVA_EINVAL, "too many elements for one step");
     int dev = 0;
     ENOVA_TRY(hipGetDevice(&dev), "hipGetDevice");

@@ -6,6 +6,20 @@
 
 namespace enova {
 
+// A launch holds fewer than 2^32 threads: a longer grid goes in runs of 2^31, launch(first block, blocks) each.
+template <class F>
+hipError_t launch_in_runs(int64_t blocks, int threads, F launch)
+{
+    const int64_t run = (int64_t{1} << 31) / threads;
+    for (int64_t from = 0; from < blocks; from += run) {
+        launch(from, static_cast<unsigned>(blocks - from < run ? blocks - from : run));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
+}
+
 // ---------------------------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------------------------

@@ -25,9 +25,9 @@ hipError_t launch_bf16(const MmParams &p, int tile, hipStream_t st)
 
 // Eight columns a thread.
 template <int EPI>
-__device__ __forceinline__ void mm_finish(const MmParams &p)
+__device__ __forceinline__ void mm_finish(const MmParams &p, int64_t from)
 {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t i = (from + blockIdx.x) * 256 + threadIdx.x;
     const int per = p.n8 / 8;
     const int64_t m = i / per, plane = static_cast<int64_t>(p.m) * p.n8;
     const int n = static_cast<int>(i - m * per) * 8;
@@ -74,14 +74,14 @@ __device__ __forceinline__ void mm_finish(const MmParams &p)
 }
 
 template <int EPI>
-__global__ void __launch_bounds__(256) k_mm_finish(MmParams p)
+__global__ void __launch_bounds__(256) k_mm_finish(MmParams p, int64_t from)
 {
-    mm_finish<EPI>(p);
+    mm_finish<EPI>(p, from);
 }
 __global__ void __launch_bounds__(256) k_mm_finish_pair(MmPair pair)
 {
     if (pair.p[blockIdx.y].slices > 1)
-        mm_finish<kMmStore>(pair.p[blockIdx.y]);
+        mm_finish<kMmStore>(pair.p[blockIdx.y], 0);
 }
 
 __global__ void __launch_bounds__(256) k_zero(uint16_t *p, int64_t n)
@@ -93,10 +93,10 @@ __global__ void __launch_bounds__(256) k_zero(uint16_t *p, int64_t n)
 
 // Eight columns a thread; a block row for each matrix.
 template <class T>
-__global__ void __launch_bounds__(256) k_pack(PackJobs jobs)
+__global__ void __launch_bounds__(256) k_pack(PackJobs jobs, int64_t from)
 {
     const PackJob j = jobs.job[blockIdx.y];
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t i = (from + blockIdx.x) * 256 + threadIdx.x;
     const int per = j.pitch / 8;
     const int64_t r = i / per;
     const int c = static_cast<int>(i - r * per) * 8;
@@ -124,6 +124,8 @@ MmPlan mm_plan(int64_t m, int64_t n, int64_t slabs, bool columns, double moves, 
         const int64_t tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile), room = tile == 256 ? 256 : 512;
         for (int64_t slices = 1; slices <= 64 && slices * 2 <= std::max<int64_t>(slabs, 2); ++slices) {
             const int64_t blocks = tiles * slices, rounds = (blocks + room - 1) / room;
+            if (blocks * (tile == 256 ? 512 : 256) >= int64_t{1} << 32)      // more threads than a launch holds
+                break;
             const double one = tile == 256 ? 1.45 : (blocks <= 256 ? 0.55 : 0.86) * (columns ? 1.35 : 1.0);
             const double mn = static_cast<double>(m) * static_cast<double>(n), used = std::min<double>(1.0, blocks / 256.0);
             double us = static_cast<double>(rounds) * (static_cast<double>((slabs + slices - 1) / slices) * one + (tile == 256 ? 11.0 : 9.0));
@@ -183,20 +185,24 @@ hipError_t launch_mm_pair(const MmPair &pair, int tile, hipStream_t st)
 
 hipError_t launch_mm_finish(const MmParams &p, MmEpilogue epi, hipStream_t st)
 {
-    const unsigned n = static_cast<unsigned>((static_cast<int64_t>(p.m) * (p.n8 / 8) + 255) / 256);
+    const auto run = [&](auto kernel) {
+        return launch_in_runs((static_cast<int64_t>(p.m) * (p.n8 / 8) + 255) / 256, 256, [&](int64_t from, unsigned n) {
+            kernel<<<n, 256, 0, st>>>(p, from);
+        });
+    };
     switch (epi) {
-    case kMmGate: k_mm_finish<kMmGate><<<n, 256, 0, st>>>(p); break;
-    case kMmGateBack: k_mm_finish<kMmGateBack><<<n, 256, 0, st>>>(p); break;
-    case kMmInt8: k_mm_finish<kMmInt8><<<n, 256, 0, st>>>(p); break;
-    default: k_mm_finish<kMmStore><<<n, 256, 0, st>>>(p); break;
+    case kMmGate: return run(k_mm_finish<kMmGate>);
+    case kMmGateBack: return run(k_mm_finish<kMmGateBack>);
+    case kMmInt8: return run(k_mm_finish<kMmInt8>);
+    default: return run(k_mm_finish<kMmStore>);
     }
-    return hipGetLastError();
 }
 
 hipError_t launch_zero(void *p, int64_t bytes, hipStream_t st)
 {
-    k_zero<<<static_cast<unsigned>((bytes / 2 + 255) / 256), 256, 0, st>>>(static_cast<uint16_t *>(p), bytes / 2);
-    return hipGetLastError();
+    return launch_in_runs((bytes / 2 + 255) / 256, 256, [&](int64_t from, unsigned n) {
+        k_zero<<<n, 256, 0, st>>>(static_cast<uint16_t *>(p) + from * 256, bytes / 2 - from * 256);
+    });
 }
 
 hipError_t launch_pack(const PackJobs &jobs, int dtype, hipStream_t st)
@@ -204,14 +210,12 @@ hipError_t launch_pack(const PackJobs &jobs, int dtype, hipStream_t st)
     int64_t most = 0;
     for (int i = 0; i < jobs.n; ++i)
         most = std::max(most, (jobs.job[i].rows * (jobs.job[i].pitch / 8) + 255) / 256);
-    if (most == 0)
-        return hipSuccess;
-    const dim3 grid(static_cast<unsigned>(most), jobs.n);
-    if (dtype == ENOVA_F32)
-        k_pack<float><<<grid, 256, 0, st>>>(jobs);
-    else
-        k_pack<__bf16><<<grid, 256, 0, st>>>(jobs);
-    return hipGetLastError();
+    return launch_in_runs(most, 256, [&](int64_t from, unsigned n) {
+        if (dtype == ENOVA_F32)
+            k_pack<float><<<dim3(n, jobs.n), 256, 0, st>>>(jobs, from);
+        else
+            k_pack<__bf16><<<dim3(n, jobs.n), 256, 0, st>>>(jobs, from);
+    });
 }
 
 }  // namespace enova

@@ -50,16 +50,18 @@ __global__ void __launch_bounds__(THREADS) k_quantize(const T *x, int64_t ld, in
 template <class T>
 hipError_t quantize(const T *x, int64_t ld, int64_t rows, int cols, int gate, int8_t *q, int pitch, float *scale, hipStream_t st)
 {
-    const unsigned n = static_cast<unsigned>(rows);
+    const auto run = [&](auto kernel, int threads) {
+        return launch_in_runs(rows, threads, [&](int64_t from, unsigned n) {
+            kernel<<<n, threads, 0, st>>>(x + from * ld, ld, cols, gate, q + from * pitch, pitch, scale + from);
+        });
+    };
     if (pitch <= 2048)
-        k_quantize<T, 256, 1><<<n, 256, 0, st>>>(x, ld, cols, gate, q, pitch, scale);
-    else if (pitch <= 4096)
-        k_quantize<T, 512, 1><<<n, 512, 0, st>>>(x, ld, cols, gate, q, pitch, scale);
-    else if (pitch <= 8192)
-        k_quantize<T, 512, 2><<<n, 512, 0, st>>>(x, ld, cols, gate, q, pitch, scale);
-    else
-        k_quantize<T, 512, 0><<<n, 512, 0, st>>>(x, ld, cols, gate, q, pitch, scale);
-    return hipGetLastError();
+        return run(k_quantize<T, 256, 1>, 256);
+    if (pitch <= 4096)
+        return run(k_quantize<T, 512, 1>, 512);
+    if (pitch <= 8192)
+        return run(k_quantize<T, 512, 2>, 512);
+    return run(k_quantize<T, 512, 0>, 512);
 }
 
 }  // namespace

@@ -187,14 +187,14 @@ __device__ __forceinline__ float2 row_stats(const float (&v)[P][kPiece], const i
 }
 
 template <class T, int TEAM, int P>
-__global__ void __launch_bounds__(block_threads<TEAM>()) k_resnorm_forward(NormParams p)
+__global__ void __launch_bounds__(block_threads<TEAM>()) k_resnorm_forward(NormParams p, int64_t first_block)
 {
     __shared__ float2 shared[2][16];
     constexpr int kTeams = block_threads<TEAM>() / TEAM;
     if (TEAM > 16)
         __builtin_assume(p.model >= kPiece);
     const int t = threadIdx.x % TEAM;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + threadIdx.x / TEAM;
+    const int64_t row = (first_block + blockIdx.x) * kTeams + threadIdx.x / TEAM;
     if (row >= p.rows)                 // a whole team
         return;
     const int64_t at = row * p.model;
@@ -607,8 +607,9 @@ template <class T, int TEAM, int P>
 hipError_t launch_forward(const NormParams &p, hipStream_t st)
 {
     constexpr int kThreads = block_threads<TEAM>(), kTeams = kThreads / TEAM;
-    k_resnorm_forward<T, TEAM, P><<<static_cast<unsigned>((p.rows + kTeams - 1) / kTeams), kThreads, 0, st>>>(p);
-    return hipGetLastError();
+    return launch_in_runs((p.rows + kTeams - 1) / kTeams, kThreads, [&](int64_t from, unsigned n) {
+        k_resnorm_forward<T, TEAM, P><<<n, kThreads, 0, st>>>(p, from);
+    });
 }
 
 // A power of two of pieces, one a thread, up to 4096 columns; three a thread where the columns fill no more than 3/4 of

@@ -734,14 +734,14 @@ hipError_t launch_mm_tail(const MmParams &p, unsigned blocks, hipStream_t st)
     return hipGetLastError();
 }
 
-// Fills in p's tiles; the number of its blocks, or 0 where that is too large.
+// Fills in p's tiles; the number of its blocks, or 0 where a launch does not hold them.
 template <class C, int BM>
 int mm_blocks(MmParams &p)
 {
     p.tiles_m = (p.m + BM - 1) / BM;
     p.tiles_n = (p.n + C::kCols - 1) / C::kCols;
     const int64_t blocks = static_cast<int64_t>(p.tiles_m) * p.tiles_n * p.slices;
-    return blocks > 0x7fffffff ? 0 : static_cast<int>(blocks);
+    return blocks * C::kThreads >= int64_t{1} << 32 ? 0 : static_cast<int>(blocks);
 }
 
 template <class MM, int EPI, int XL, int WL, int BM, int BN, int WM, int WN>

@@ -182,3 +182,43 @@ def test_norms_in_place(model, dtype, post):
         torch.cuda.current_stream().cuda_stream)
     assert status == binding.ENOVA_OK
     assert all(torch.equal(a, b) for a, b in zip((res, out, stats), want))
+
+
+# ----------------------------------------------------------------------------- long calls
+def windows_of(rows, run):
+    """Row ranges at both ends and around the places where one launch's rows end."""
+    return [slice(max(at - 40, 0), min(at + 40, rows)) for at in (0, run, rows // 2, rows)]
+
+
+def test_int8_product_of_more_rows_than_a_launch_has_threads_for():
+    rows = (1 << 24) + 5                       # blocks of 256 threads, one a row
+    g = rng(8)
+    codes, scales = blocks.quantize_weight(normal(g, 8, 16).float().cuda())
+    op = blocks.Int8Linear(codes, scales)
+    x = torch.randn(rows, 16, dtype=torch.bfloat16, device="cuda")
+    y = op(x)
+    for s in windows_of(rows, 1 << 23):
+        assert torch.equal(y[s], op(x[s]))
+
+
+def test_norms_of_more_rows_than_a_launch_has_threads_for():
+    rows = (1 << 28) + 5                       # teams of 16 threads
+    op = blocks.ResidualNorm(2, group=3)
+    post, pre = (torch.tensor([0.5, 2.0], device="cuda") for _ in range(2))
+    residual, branch = (torch.randn(rows, 2, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    gate = torch.randn(-(-rows // 3), 2, device="cuda")
+    got = op.forward(residual, branch, post, pre, gate=gate)
+    for s in windows_of(rows, 1 << 27):
+        first = s.start // 3 * 3
+        part = op.forward(residual[first:s.stop], branch[first:s.stop], post, pre, gate=gate[first // 3:-(-s.stop // 3)])
+        assert all(torch.equal(a[first:s.stop], b) for a, b in zip(got, part))
+
+
+def test_gradients_of_no_rows_are_zeros_in_all_of_a_large_weight():
+    model, hidden = 1 << 16, (1 << 16) + 1
+    op = blocks.GatedBlock(model, hidden)
+    dw = torch.full((model, hidden), 1.0, dtype=torch.bfloat16, device="cuda")
+    w = dw.data_ptr()                          # of no rows nothing is read
+    status = binding.lib().enova_gated_backward(op.handle, None, model, 0, w, w, w, None, None, model, None, model, None,
+                                                None, w, torch.cuda.current_stream().cuda_stream)
+    assert status == binding.ENOVA_OK and not dw.any()
