@@ -5,6 +5,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <limits>
 #include <new>
 #include <vector>
 
@@ -917,7 +918,8 @@ enova_status enova_adamw_step(enova_adamw op, int64_t n, double lr, float grad_s
     a.keep = static_cast<float>(1.0 - lr * c.decay);
     a.lr = static_cast<float>(lr * (1.0 / (1.0 - std::pow(c.b1, static_cast<double>(n)))));
     a.root = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(c.b2, static_cast<double>(n))));
-    a.eps = static_cast<float>(c.eps);
+    // the kernel's reciprocal takes no subnormal numbers; beside a root of v in fp32 (3.7e-23 at least) neither does eps show
+    a.eps = std::max(static_cast<float>(c.eps), std::numeric_limits<float>::min());
     a.grad_scale = grad_scale;
     a.step = static_cast<uint32_t>(n);
     ENOVA_TRY(launch_adamw(c.bits, c.param_dtype, c.grad_dtype, op->d_tensors, op->d_chunks, op->chunks, a, stream), "AdamW step");

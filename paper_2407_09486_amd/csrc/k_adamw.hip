@@ -181,7 +181,7 @@ __device__ __forceinline__ void adam_block(const AdamTensor &t, const AdamArgs &
         m[e] = m[e] * a.b1 + ge * a.b1c;
         v[e] = v[e] * a.b2 + (ge * ge) * a.b2c;
         r[e] = sqrtf(v[e]);
-        // the parameter's own rounding is 10^4 times what the quotient's last bit is to it
+        // the reciprocal is within an ulp, so the update is within two of the formula's in fp32
         l.p[e] = l.p[e] * a.keep - (m[e] * a.lr) * __builtin_amdgcn_rcpf(r[e] * a.root + a.eps);
     }
     store4(static_cast<P *>(t.param), at, left, wide, l.p);

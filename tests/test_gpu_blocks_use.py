@@ -222,3 +222,18 @@ def test_gradients_of_no_rows_are_zeros_in_all_of_a_large_weight():
     status = binding.lib().enova_gated_backward(op.handle, None, model, 0, w, w, w, None, None, model, None, model, None,
                                                 None, w, torch.cuda.current_stream().cuda_stream)
     assert status == binding.ENOVA_OK and not dw.any()
+
+
+# ----------------------------------------------------------------------------- AdamW
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-50, 1e-42, 1.2e-38, 1e-8])
+def test_adamw_of_gradients_that_are_zero(eps, bits):
+    """However small eps is, an element without a gradient only decays, and the others step by lr."""
+    g = rng(4)
+    p = normal(g, 1000).float().cuda()
+    d = normal(g, 1000).float().cuda()
+    d[::3] = 0.0
+    want = p.double() * (1 - 1e-2 * 0.01) - torch.sign(d.double()) * 1e-2 * (d.abs() / (d.abs() + eps)).nan_to_num()
+    op = blocks.AdamW([p], [d], bits=bits, eps=eps, lr=1e-2)
+    op.step()
+    assert (p.double() - want).abs().max() <= 4 * 2.0 ** -24 * 4      # p of up to 4
