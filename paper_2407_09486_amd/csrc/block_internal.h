@@ -137,7 +137,7 @@ struct MmParams {
     int m2, m1;                        // kMmStore: rows m1 .. m2 - 1 are padding and written nowhere
     int64_t plane;                     // elements between the three bf16 parts of an fp32 operand (0: bf16)
     float *h32;                        // kMmGate of few rows of fp32: h in fp32, pitch ldg (c may then be NULL)
-    int f32;                           // type of c (kMmStore, kMmInt8): fp32 instead of bf16
+    int f32;                           // the handle's type, and c's (kMmStore, kMmInt8): fp32 instead of bf16
     int wide;                          // rows of c are aligned for eight elements at a time
     // saved projections, pitch ldg, zeros past n: fp32, or where ge and ue are there f16 with an exponent for every
     // eight neighbouring columns (pitch ldg / 8)

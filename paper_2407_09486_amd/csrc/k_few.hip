@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_mm_few(MmParams p)
             gv[e] = sum[0][e];
             uv[e] = sum[1][e];
         }
-        gate_acts(p.act, gv, h, da);
+        gate_acts<std::is_same_v<T, float>>(p.act, gv, h, da);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             h[e] *= sum[1][e];

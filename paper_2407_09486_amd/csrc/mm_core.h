@@ -49,10 +49,14 @@ static __device__ const uint4 mm_zero = {0u, 0u, 0u, 0u};
 struct Bf16Mm {
     typedef mm_f4 Acc;
     static constexpr int kElem = 2;
+    static constexpr bool kExact = false;      // activations (gate_act)
     __device__ static Acc mma(uint4 a, uint4 b, Acc c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mm_bf8, a), __builtin_bit_cast(mm_bf8, b), c, 0, 0, 0);
     }
+};
+struct PartsMm : Bf16Mm {              // of fp32 operands in three parts
+    static constexpr bool kExact = true;
 };
 struct Int8Mm {
     typedef mm_i4 Acc;
@@ -174,21 +178,35 @@ struct Fragments {
     }
 };
 
-// act(g) and its derivative. The hardware's exponential and reciprocal (1 ulp each) and, for GELU, Phi from
-// Abramowitz and Stegun's formula 7.1.26 for erf (1.5e-7 at most, sharing the exponential with the density): errors
-// of an fp32 rounding of values near 1. With the library's expf, erff and division a tile of the hidden gradient
-// spent as long on them as on memory (16384 x 4096 -> 8192: 1019 us, 996 us so).
-template <int ACT>
+// act(g) and its derivative. EXACT (blocks of fp32): within a few ulp of the result, GELU with expf and erfcf. Else (bf16,
+// whose next rounding is 2^-9, and 8-bit codes) the hardware's exponential and reciprocal, an ulp each, the former of a
+// rounded product (a relative |g| 2^-24 more), and for GELU Phi from Abramowitz and Stegun's formula 7.1.26 for erf,
+// sharing the exponential with the density: within 2.5e-7, which is no more than the order of the tail where g < -5.
+// With expf, erff and division a tile of the bf16 hidden gradient spent as long on them as on memory
+// (16384 x 4096 -> 8192: 1019 us, 996 us so).
+template <int ACT, bool EXACT>
 __device__ __forceinline__ void gate_act(float g, float &a, float &da)
 {
-    constexpr float kLog2e = 1.4426950408889634f;
+    constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = 1.4426950408889634 - kLog2e;
     if constexpr (ACT == ENOVA_GATE_RELU) {
         a = g < 0.0f ? 0.0f : g;
         da = g > 0.0f ? 1.0f : 0.0f;
+    } else if constexpr (ACT == ENOVA_GATE_SILU && EXACT) {
+        // e^-g as 2^t (1 + r ln 2), r what the product t lost; beyond |g| = 128 it is 0 or infinite all the same
+        const float x = fminf(fmaxf(g, -128.0f), 128.0f), t = -kLog2e * x;
+        const float r = __builtin_fmaf(-kLog2e, x, -t) - kLog2eRest * x, p = __builtin_amdgcn_exp2f(t);
+        const float e = p < __builtin_inff() ? __builtin_fmaf(p, r * 0.6931471805599453f, p) : p;
+        const float s = __builtin_amdgcn_rcpf(1.0f + e);
+        a = g * s;
+        da = s * (1.0f + g * (g < 0.0f ? 1.0f - s : e * s));
     } else if constexpr (ACT == ENOVA_GATE_SILU) {
         const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * g));
         a = g * s;
         da = s * (1.0f + g * (1.0f - s));
+    } else if constexpr (EXACT) {
+        const float cdf = 0.5f * erfcf(-0.70710678118654752f * g);
+        a = g * cdf;
+        da = cdf + g * expf(-0.5f * g * g) * 0.39894228040143268f;
     } else {
         const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678118654752f * fabsf(g));
         const float e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * g * g);
@@ -198,22 +216,13 @@ __device__ __forceinline__ void gate_act(float g, float &a, float &da)
         da = cdf + g * e * 0.39894228040143268f;
     }
 }
-__device__ __forceinline__ void gate_act(int act, float g, float &a, float &da)
-{
-    if (act == ENOVA_GATE_SILU)
-        gate_act<ENOVA_GATE_SILU>(g, a, da);
-    else if (act == ENOVA_GATE_GELU)
-        gate_act<ENOVA_GATE_GELU>(g, a, da);
-    else
-        gate_act<ENOVA_GATE_RELU>(g, a, da);
-}
-template <int N>
+template <bool EXACT, int N>
 __device__ __forceinline__ void gate_acts(int act, const float (&g)[N], float (&a)[N], float (&da)[N])
 {
     const auto all = [&](auto which) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            gate_act<decltype(which)::value>(g[e], a[e], da[e]);
+            gate_act<decltype(which)::value, EXACT>(g[e], a[e], da[e]);
     };
     if (act == ENOVA_GATE_SILU)
         all(std::integral_constant<int, ENOVA_GATE_SILU>());
@@ -335,6 +344,7 @@ struct SavedPiece {
 };
 
 // What becomes of eight neighbouring columns n .. n + 7 of a finished row.
+template <bool EXACT>
 __device__ __forceinline__ void finish_gate(const MmParams &p, int64_t m, int n, float (&g)[8], float (&u)[8])
 {
     float h[8], da[8];
@@ -343,7 +353,7 @@ __device__ __forceinline__ void finish_gate(const MmParams &p, int64_t m, int n,
         g[e] = n + e < p.n ? g[e] : 0.0f;
         u[e] = n + e < p.n ? u[e] : 0.0f;
     }
-    gate_acts(p.act, g, h, da);
+    gate_acts<EXACT>(p.act, g, h, da);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         h[e] *= u[e];
@@ -363,11 +373,12 @@ __device__ __forceinline__ void finish_gate(const MmParams &p, int64_t m, int n,
         store8(static_cast<float *>(p.u) + m * p.ldg + n, u);
     }
 }
+template <bool EXACT>
 __device__ __forceinline__ void finish_gate_back(const MmParams &p, int64_t m, int n, const float (&dh)[8], const float (&g)[8],
                                                  const float (&u)[8])
 {
     float dg[8], du[8], a[8], da[8];
-    gate_acts(p.act, g, a, da);
+    gate_acts<EXACT>(p.act, g, a, da);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float d = n + e < p.n ? dh[e] : 0.0f;
@@ -695,11 +706,11 @@ __device__ __forceinline__ void mm_block(const MmParams &p, int block)
                         *reinterpret_cast<Acc *>(to + static_cast<int64_t>(p.m) * p.n8 + e) = Acc{v2[e], v2[e + 1], v2[e + 2], v2[e + 3]};
                 }
             } else if constexpr (EPI == kMmGate) {
-                finish_gate(p, m, n, v, v2);
+                finish_gate<MM::kExact>(p, m, n, v, v2);
             } else if constexpr (EPI == kMmGateBack) {
                 float g[8], u[8];
                 saved.values(p, g, u);
-                finish_gate_back(p, m, n, v, g, u);
+                finish_gate_back<MM::kExact>(p, m, n, v, g, u);
             } else if constexpr (EPI == kMmInt8) {
                 finish_int8<8>(p, m, n, v, columns);
             } else {

@@ -38,7 +38,7 @@ __device__ __forceinline__ void quant_values(const T *row, int c, int cols, int 
     if (gate >= 0) {
         float a[8], da[8], u[8];
         load_x8(row + cols, c, cols, u);
-        gate_acts(gate, v, a, da);
+        gate_acts<false>(gate, v, a, da);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             v[i] = a[i] * u[i];

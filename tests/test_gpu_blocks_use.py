@@ -237,3 +237,28 @@ def test_adamw_of_gradients_that_are_zero(eps, bits):
     op = blocks.AdamW([p], [d], bits=bits, eps=eps, lr=1e-2)
     op.step()
     assert (p.double() - want).abs().max() <= 4 * 2.0 ** -24 * 4      # p of up to 4
+
+
+# ----------------------------------------------------------------------------- activations
+@pytest.mark.parametrize("rows", [60, 3001])
+@pytest.mark.parametrize("act,ends", [("gelu", 11.0), ("silu", 70.0)])
+def test_block_f32_activations_are_those_of_fp32(act, ends, rows):
+    """act(g) and act'(g) by themselves, through weights of 0 and 1, far into the tail.
+
+    GELU: erfc of a product rounded once and of a rounded constant is off by 2 (g^2 / 2) 1.3 units of 2^-24, the
+    function and the products by a few more. SiLU: an exponential, a sum, a quotient and a product. The derivatives
+    are sums of such terms up to 1.1 in size."""
+    g = torch.linspace(-ends, ends, rows, device="cuda")
+    x = torch.stack([g, torch.ones_like(g)], 1)
+    wg, wu, wd = (torch.tensor(w, device="cuda") for w in ([[1.0, 0.0]], [[0.0, 1.0]], [[1.0], [0.0]]))
+    dy = torch.zeros_like(x)
+    dy[:, 0] = 1.0
+    y, dx, *_ = run_block(blocks.GatedBlock(2, 1, dtype="f32", act=act), x, wg, wu, wd, dy)
+    v = g.double().requires_grad_(True)
+    a = 0.5 * v * torch.special.erfc(-v / 2 ** 0.5) if act == "gelu" else v * torch.sigmoid(v)
+    da, = torch.autograd.grad(a.sum(), v)
+    a, v = a.detach(), v.detach()
+    tol = (8 + (2 * v * v if act == "gelu" else 0)) * 2.0 ** -24 * a.abs()
+    assert ((y[:, 0].double() - a).abs() <= tol).all()
+    assert ((dx[:, 1].double() - a).abs() <= tol).all()
+    assert (dx[:, 0].double() - da).abs().max() <= 1e-6
