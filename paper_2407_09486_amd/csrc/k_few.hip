@@ -208,8 +208,8 @@ __global__ void __launch_bounds__(WAVES * 64) k_mm_few(MmParams p)
         if (p.ge) {                    // the other four of eight columns are 16 lanes away
             const float tg = finite_top(gv), tu = finite_top(uv);
             const int eg = coded_exponent(fmaxf(tg, __shfl_xor(tg, 16))), eu = coded_exponent(fmaxf(tu, __shfl_xor(tu, 16)));
-            store_coded(p.g, at, gv, eg);
-            store_coded(p.u, at, uv, eu);
+            store_coded<true>(p.g, at, gv, eg);
+            store_coded<false>(p.u, at, uv, eu);
             if (g % 2 == 0) {
                 p.ge[at / 8] = static_cast<int8_t>(eg);
                 p.ue[at / 8] = static_cast<int8_t>(eu);

@@ -287,15 +287,19 @@ __device__ __forceinline__ float finite_top(const float (&v)[N])
     }
     return top;
 }
-// N values under exponent e
-template <int N>
+// N values under exponent e. SIGNED (g): a zero's sign bit says that the value was not positive. One that was, but is
+// nothing beside its neighbours, comes back as the smallest normal number: ReLU's derivative is 1 there.
+template <bool SIGNED, int N>
 __device__ __forceinline__ void store_coded(void *dst, int64_t at, const float (&v)[N], int e)
 {
     const float by = power_of_two(14 - e);
     _Float16 h[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
         h[i] = static_cast<_Float16>(v[i] * by);
+        if (SIGNED)
+            h[i] = v[i] > 0.0f ? h[i] : -__builtin_fabsf16(h[i]);
+    }
     typedef uint32_t pack __attribute__((ext_vector_type(N / 2)));
     *reinterpret_cast<pack *>(static_cast<_Float16 *>(dst) + at) = __builtin_bit_cast(pack, h);
 }
@@ -322,11 +326,13 @@ struct SavedPiece {
     {
         if (p.ge) {
             typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+            typedef uint16_t bits8 __attribute__((ext_vector_type(8)));
             const half8 hg = __builtin_bit_cast(half8, q[0]), hu = __builtin_bit_cast(half8, q[1]);
+            const bits8 bits = __builtin_bit_cast(bits8, q[0]);
             const float bg = power_of_two(eg - 14), bu = power_of_two(eu - 14);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                g[e] = static_cast<float>(hg[e]) * bg;
+                g[e] = bits[e] ? static_cast<float>(hg[e]) * bg : 0x1p-126f;
                 u[e] = static_cast<float>(hu[e]) * bu;
             }
         } else {
@@ -364,8 +370,8 @@ __device__ __forceinline__ void finish_gate(const MmParams &p, int64_t m, int n,
     if (p.ge) {
         const int64_t at = m * p.ldg + n;
         const int eg = coded_exponent(finite_top(g)), eu = coded_exponent(finite_top(u));
-        store_coded(p.g, at, g, eg);
-        store_coded(p.u, at, u, eu);
+        store_coded<true>(p.g, at, g, eg);
+        store_coded<false>(p.u, at, u, eu);
         p.ge[at / 8] = static_cast<int8_t>(eg);
         p.ue[at / 8] = static_cast<int8_t>(eu);
     } else if (p.g) {

@@ -6,7 +6,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from paper_2407_09486_amd import binding  # noqa: E402
-from test_gpu_blocks import block_inputs, blocks, norm_inputs, normal, rng, run_block, run_norm  # noqa: E402
+from test_gpu_blocks import block64, block_inputs, blocks, close, norm_inputs, normal, rng, run_block, run_norm  # noqa: E402
 
 
 # ----------------------------------------------------------------------------- graphs
@@ -262,3 +262,23 @@ def test_block_f32_activations_are_those_of_fp32(act, ends, rows):
     assert ((y[:, 0].double() - a).abs() <= tol).all()
     assert ((dx[:, 1].double() - a).abs() <= tol).all()
     assert (dx[:, 0].double() - da).abs().max() <= 1e-6
+
+
+@pytest.mark.parametrize("saved", [True, False])
+@pytest.mark.parametrize("rows", [20, 300])
+def test_block_relu_derivative_of_a_small_g_beside_large_ones(rows, saved):
+    """A hidden unit whose g is 2^-50 of its neighbours' is as much on as they are (its own value is kept to 2^-39 of
+    the largest: nothing)."""
+    t = block_inputs(rows, 8, 16, "bf16", rows)
+    t[0].abs_()
+    t[1].abs_().add_(0.1)
+    t[1][3] *= 2.0 ** -50
+    t[1][12] *= -(2.0 ** -50)
+    got = run_block(blocks.GatedBlock(8, 16, act="relu"), *t, saved=saved)
+    want = block64(*t, "relu")
+    for unit in range(16):
+        close(got[2][unit], want[2][unit], 2e-2, f"dwg[{unit}]")
+        if unit != 3:
+            close(got[3][unit], want[3][unit], 2e-2, f"dwu[{unit}]")
+    assert float(got[3][3].abs().max()) <= 2.0 ** -38 * float(want[3].abs().max())
+    assert not got[2][12].any() and not got[3][12].any()
