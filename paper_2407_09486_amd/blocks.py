@@ -273,12 +273,11 @@ class AdamW(_Handle):
         self.steps += 1
 
     def states(self, m=None, v=None, stream=None):
-        """The values of m and v in fp32 (into the lists given): for checkpoints, and to look at 8-bit states."""
+        """The values of m and v in fp32, into the lists given: for checkpoints, and to look at 8-bit states."""
         if self.bits == 32 and m is None and v is None:
             return self.m, self.v
-        if m is None or v is None:
-            with _on(stream):
-                m, v = ([torch.empty_like(p, dtype=torch.float32) for p in self.params] for _ in range(2))
+        with _on(stream):
+            m, v = ([torch.empty_like(p, dtype=torch.float32) for p in self.params] if t is None else t for t in (m, v))
         pm, pv = (self._flat(t, (torch.float32,), "states", self._sizes) for t in (m, v))
         n = len(pm)
         _check(lib().enova_adamw_states(self.handle, (ctypes.c_void_p * n)(*pm), (ctypes.c_void_p * n)(*pv),

@@ -282,3 +282,16 @@ def test_block_relu_derivative_of_a_small_g_beside_large_ones(rows, saved):
             close(got[3][unit], want[3][unit], 2e-2, f"dwu[{unit}]")
     assert float(got[3][3].abs().max()) <= 2.0 ** -38 * float(want[3].abs().max())
     assert not got[2][12].any() and not got[3][12].any()
+
+
+def test_adamw_states_into_one_list_given():
+    g = rng(4)
+    p = [normal(g, n).float().cuda() for n in (1000, 7)]
+    op = blocks.AdamW(p, [a * 0.1 for a in p], bits=8)
+    op.step()
+    want = op.states()
+    for which in (0, 1):
+        mine = [torch.full_like(a, 9.0) for a in p]
+        got = op.states(**{"mv"[which]: mine})
+        assert all(a is b for a, b in zip(got[which], mine))
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
