@@ -7,6 +7,7 @@ missing this module raises instead of falling back to anything else.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -209,6 +210,17 @@ def _stream(stream):
     import torch
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
+
+
+_CURRENT = contextlib.nullcontext()
+
+
+def _on(stream):
+    """Where a call's results are allocated: on the stream that writes them."""
+    if stream is None:
+        return _CURRENT
+    import torch
+    return torch.cuda.stream(stream)
 
 
 # ----------------------------------------------------------------------------- C entry points
@@ -463,8 +475,9 @@ class ConfigScanner:
         import torch
         dev = x.device
         n = stream_offsets.numel() - 1
-        f = [torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows] for _ in range(5)]
-        sig = torch.empty(max(n_windows, 1), dtype=torch.uint8, device=dev)[:n_windows]
+        with _on(stream):
+            f = [torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows] for _ in range(5)]
+            sig = torch.empty(max(n_windows, 1), dtype=torch.uint8, device=dev)[:n_windows]
         _check(lib().enova_config_scan(ctypes.c_void_p(self.handle), _dptr(x), _dptr(stream_offsets),
                                        _dptr(window_offsets), n, int(n_windows), _dptr(f[0]), _dptr(f[1]),
                                        _dptr(f[2]), _dptr(sig), _dptr(f[3]), _dptr(f[4]), _stream(stream)),
@@ -476,8 +489,9 @@ class ConfigScanner:
         import torch
         dev = x.device
         n = stream_offsets.numel() - 1
-        sig = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)[:n]
-        d = [torch.empty(max(n, 1), dtype=torch.float64, device=dev)[:n] for _ in range(4)]
+        with _on(stream):
+            sig = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)[:n]
+            d = [torch.empty(max(n, 1), dtype=torch.float64, device=dev)[:n] for _ in range(4)]
         _check(lib().enova_config_recommend(ctypes.c_void_p(self.handle), _dptr(x), _dptr(stream_offsets), n,
                                             _dptr(sig), _dptr(d[0]), _dptr(d[1]), _dptr(d[2]), _dptr(d[3]),
                                             _stream(stream)),
@@ -517,7 +531,8 @@ def make_config(metrics, window, stride, hidden, latent=16, dtype="f32", act="re
 
 
 class Detector:
-    """Owns one library handle; methods call the C entry points on torch's current stream."""
+    """Owns one library handle; methods call the C entry points on torch's current stream, or on the one given, to
+    which their results then belong."""
 
     def __init__(self, metrics, window, stride, hidden, weights: dict, latent=16, dtype="f32",
                  act="relu", kernel="auto", ref_frac=0.5):
@@ -556,9 +571,10 @@ class Detector:
         import torch
         dev = x.device
         n = stream_offsets.numel() - 1
-        scores = torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows]
-        mdv = torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows] if md else None
-        fl = torch.empty(max(n_windows, 1), dtype=torch.uint8, device=dev)[:n_windows] if flags else None
+        with _on(stream):
+            scores = torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows]
+            mdv = torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows] if md else None
+            fl = torch.empty(max(n_windows, 1), dtype=torch.uint8, device=dev)[:n_windows] if flags else None
         enova_detect_score(self.handle, x, stream_offsets, window_offsets, n, n_windows, ref_mean, ref_std,
                            threshold, scores, mdv, fl, stream)
         return scores, mdv, fl
@@ -572,9 +588,10 @@ class Detector:
         n = stream_offsets.numel() - 1
         M = self.cfg.metrics
         k = 1 if scores_only else 3
-        f = [torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows] for _ in range(k)]
-        f += [None] * (3 - k)
-        mdm = None if scores_only else torch.empty((max(n_windows, 1), M), dtype=torch.float32, device=dev)[:n_windows]
+        with _on(stream):
+            f = [torch.empty(max(n_windows, 1), dtype=torch.float32, device=dev)[:n_windows] for _ in range(k)]
+            f += [None] * (3 - k)
+            mdm = None if scores_only else torch.empty((max(n_windows, 1), M), dtype=torch.float32, device=dev)[:n_windows]
         enova_detect_score_ext(self.handle, x, stream_offsets, window_offsets, n, n_windows, ref_mean, ref_std,
                                {"reference": ENOVA_NORM_REFERENCE, "window": ENOVA_NORM_WINDOW}[norm], f[0], f[1],
                                mdm, f[2], stream)
@@ -585,7 +602,8 @@ class Detector:
         import torch
         n = stream_offsets.numel() - 1
         nw = scores.numel()
-        fl = torch.empty(max(nw, 1), dtype=torch.uint8, device=scores.device)[:nw] if flags else None
+        with _on(stream):
+            fl = torch.empty(max(nw, 1), dtype=torch.uint8, device=scores.device)[:nw] if flags else None
         thr, info = enova_detect_threshold(self.handle, scores, stream_offsets, window_offsets, n, nw,
                                            level, q, fl, stream)
         return thr, info, fl

@@ -11,13 +11,13 @@ arguments, and keeps them until the work is done.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import numpy as np
 import torch
 
-from .binding import (ENOVA_BF16, ENOVA_F32, _check, enova_adamw_config, enova_gated_config, enova_i8_config, enova_resnorm_config, lib)
+from .binding import (ENOVA_BF16, ENOVA_F32, _check, _on, enova_adamw_config, enova_gated_config, enova_i8_config,
+                      enova_resnorm_config, lib)
 
 __all__ = ["GatedBlock", "ResidualNorm", "AdamW", "Int8Linear", "quantize_weight"]
 
@@ -31,14 +31,6 @@ def _known(value, table, what):
     if value not in table:
         raise ValueError(f"{what} {value!r}: one of {', '.join(map(repr, table))}")
     return table[value]
-
-
-_CURRENT = contextlib.nullcontext()
-
-
-def _on(stream):
-    """Where a call's results are allocated: on the stream that writes them."""
-    return _CURRENT if stream is None else torch.cuda.stream(stream)
 
 
 class _Handle:
