@@ -311,7 +311,8 @@ enova_status enova_train_init(const enova_train_config *config, const enova_dete
  * and capturing another first waits for the device. Steps taken with timing on, or with graph replay
  * off, launch their kernels one by one on `stream`, as does a step on a stream that is being
  * captured: the caller's graph then holds the step on these buffers (with timing off, and after a
- * step of this batch size or a larger one, since a capture cannot allocate). Errors: EINVAL, ENOMEM,
+ * step of this batch size or a larger one, since a capture cannot allocate; the trainer keeps those
+ * buffers when a later step needs larger ones, and has to outlive the graph). Errors: EINVAL, ENOMEM,
  * EHIP.
  */
 enova_status enova_train_step(enova_trainer t, const float *V, const float *labels, const float *eps,

@@ -7,6 +7,7 @@
 #include <cstdint>
 #include <cstring>
 #include <new>
+#include <vector>
 
 #include "enova_detect.h"
 #include "train_internal.h"
@@ -40,6 +41,9 @@ struct enova_trainer_s {
     float *kl = nullptr, *logp = nullptr;                                          // [B]
     float *work = nullptr;                                                         // split-reduction partials
     int64_t work_cap = 0;
+    // a caller's graph holds steps, and the addresses above: buffers that were outgrown since stay allocated
+    bool captured = false;
+    std::vector<void *> outgrown;
     // timing: an event pair around every product of the last step and around the whole step
     static constexpr int kMaxEvents = 2 * 16 + 2;
     bool timed = false;
@@ -93,6 +97,8 @@ void free_trainer(enova_trainer t)
     for (void *q : ptrs)
         if (q)
             (void)hipFree(q);
+    for (void *q : t->outgrown)
+        (void)hipFree(q);
     for (hipEvent_t e : t->ev)
         if (e)
             (void)hipEventDestroy(e);
@@ -133,6 +139,21 @@ int64_t workspace_floats(const enova_trainer t, int B)
     return step_work(t, B).total;
 }
 
+// Lets go of a batch buffer. One that a caller's graph may hold is kept until the trainer goes (and for good where
+// the host has no memory to note it).
+void outgrow(enova_trainer t, float *&q)
+{
+    if (!t->captured) {
+        (void)hipFree(q);
+    } else if (q) {
+        try {
+            t->outgrown.push_back(q);
+        } catch (const std::bad_alloc &) {
+        }
+    }
+    q = nullptr;
+}
+
 // Grows the batch buffers to B rows (freeing the old ones synchronises the device).
 enova_status ensure_batch(enova_trainer t, int B)
 {
@@ -140,8 +161,7 @@ enova_status ensure_batch(enova_trainer t, int B)
     const int64_t ws = workspace_floats(t, B);
     if (ws > t->work_cap) {
         ++t->gen;
-        (void)hipFree(t->work);
-        t->work = nullptr;
+        outgrow(t, t->work);
         t->work_cap = 0;
         if ((st = alloc_floats(&t->work, static_cast<size_t>(ws))) != ENOVA_OK)
             return st;
@@ -155,15 +175,14 @@ enova_status ensure_batch(enova_trainer t, int B)
     float **b2[] = {&t->ml, &t->gml};
     float **b1[] = {&t->kl, &t->logp};
     for (float **q : bh)
-        (void)hipFree(*q), *q = nullptr;
+        outgrow(t, *q);
     for (float **q : bl)
-        (void)hipFree(*q), *q = nullptr;
+        outgrow(t, *q);
     for (float **q : b2)
-        (void)hipFree(*q), *q = nullptr;
+        outgrow(t, *q);
     for (float **q : b1)
-        (void)hipFree(*q), *q = nullptr;
-    (void)hipFree(t->out);
-    t->out = nullptr;
+        outgrow(t, *q);
+    outgrow(t, t->out);
     t->cap = 0;
     for (float **q : bh)
         if ((st = alloc_floats(q, static_cast<size_t>(B) * t->H)) != ENOVA_OK)
@@ -461,6 +480,7 @@ enova_status enova_train_step(enova_trainer t, const float *V, const float *labe
     hipError_t e = hipStreamIsCapturing(s, &cap);
     if (e != hipSuccess)
         return hip_fail(e, "training step's stream");
+    t->captured |= cap != hipStreamCaptureStatusNone;
     if (t->timed || !t->use_graph || cap != hipStreamCaptureStatusNone) {
         e = launch_step_args(t->args + 1, args, s);
         if (e == hipSuccess)
