@@ -20,6 +20,11 @@ hipError_t launch_in_runs(int64_t blocks, int threads, F launch)
     return hipSuccess;
 }
 
+// 16 bytes at any address: the hardware's loads and stores take it.
+struct __attribute__((packed, aligned(1))) Any16 {
+    uint4 v;
+};
+
 // ---------------------------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------------------------
@@ -190,7 +195,7 @@ struct PackJobs {
     PackJob job[kPackJobs];
 };
 hipError_t launch_pack(const PackJobs &jobs, int dtype, hipStream_t st);
-// The 8-bit product of few rows that takes x as it is (every block makes the codes itself), where
+// The 8-bit product of a row that takes x as it is (every block makes the codes itself), where
 // i8_fused(rows, pitch) says so.
 bool i8_fused(int64_t rows, int pitch);
 struct QuantParams {

@@ -16,10 +16,6 @@ namespace {
 
 constexpr int kFewWaves = 16;          // of a block; half as many where three or four fragments of x's rows fill LDS
 
-struct __attribute__((packed, aligned(1))) Any16 {
-    uint4 v;
-};
-
 // The operand of one matrix operation as a lane holds it: 8 elements (16 of int8), as they are or in parts.
 template <class T>
 struct FewOp {
@@ -232,16 +228,16 @@ __global__ void __launch_bounds__(WAVES * 64) k_mm_few(MmParams p)
 // The 8-bit product of one row in one launch: every block makes the row's codes for itself, in LDS (it comes
 // from the caches, 16 KiB for 8192 values; the launch that would make them once takes longer than that: one row,
 // 8192 -> 4096: 24 us with it, 10.7 us so), while its weights are on their way. Four rows, one after the other, took
-// longer than the launch (8192 -> 8192: 31 us, five rows with it 19).
-constexpr int kFusedBytes = 64 * 1024, kFusedRows = 1;
+// longer than the launch (8192 -> 8192: 31 us, five rows with it 19); two and three were not tried.
+constexpr int kFusedBytes = 64 * 1024;
 
 template <class T>
 __global__ void __launch_bounds__(kFewWaves * 64) k_i8_fused(MmParams p, QuantParams x)
 {
     typedef FewOp<int8_t> Op;
-    extern __shared__ __attribute__((aligned(16))) int8_t codes[];    // [rows][pitch]
+    extern __shared__ __attribute__((aligned(16))) int8_t codes[];    // [pitch]
     __shared__ mm_i4 joined[kFewWaves][64];
-    __shared__ float tops[kFusedRows][kFewWaves], scales[kFusedRows];
+    __shared__ float tops[kFewWaves], scale;
     constexpr int kThreads = kFewWaves * 64;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane % 16, g = lane / 16;
     const int n0 = blockIdx.x * 16, pitch = p.k;
@@ -256,24 +252,22 @@ __global__ void __launch_bounds__(kFewWaves * 64) k_i8_fused(MmParams p, QuantPa
         for (int s = 0; s < 2; ++s)
             ow[a][s].load_some(w + slab * kSlab + s * 64, slab < whole ? 1 : 0);
     }
-    for (int m = 0; m < p.m; ++m) {
-        const T *const src = static_cast<const T *>(x.x) + m * x.ld;
-        float v[8] = {}, top = 0.0f;   // zeros past the row: codes of 0 there
-        for (int c = threadIdx.x * 8; c < x.cols; c += kThreads * 8) {
-            quant_values(src, c, x.cols, x.gate, v);
-            top = quant_top(v, top);
-        }
-        top = block_top<kThreads>(top, tops[m]);
-        for (int c = threadIdx.x * 8; c < pitch; c += kThreads * 8) {
-            if (x.cols > kThreads * 8)             // else v still holds them
-                quant_values(src, c, x.cols, x.gate, v);
-            *reinterpret_cast<uint2 *>(codes + m * pitch + c) = quant_codes(v, top);
-        }
-        if (threadIdx.x == 0)
-            scales[m] = quant_scale(top);
+    const T *const src = static_cast<const T *>(x.x);
+    float v[8] = {}, top = 0.0f;       // zeros past the row: codes of 0 there
+    for (int c = threadIdx.x * 8; c < x.cols; c += kThreads * 8) {
+        quant_values(src, c, x.cols, x.gate, v);
+        top = quant_top(v, top);
     }
+    top = block_top<kThreads>(top, tops);
+    for (int c = threadIdx.x * 8; c < pitch; c += kThreads * 8) {
+        if (x.cols > kThreads * 8)                 // else v still holds them
+            quant_values(src, c, x.cols, x.gate, v);
+        *reinterpret_cast<uint2 *>(codes + c) = quant_codes(v, top);
+    }
+    if (threadIdx.x == 0)
+        scale = quant_scale(top);
     __syncthreads();
-    const int8_t *const q = codes + min(i, p.m - 1) * pitch + g * 16;
+    const int8_t *const q = codes + g * 16;        // all 16 rows of the operation are this one
     mm_i4 acc = {0, 0, 0, 0};
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
@@ -307,16 +301,16 @@ __global__ void __launch_bounds__(kFewWaves * 64) k_i8_fused(MmParams p, QuantPa
     joined[wave][lane] = acc;
     __syncthreads();
     const int n = n0 + 4 * g;
-    if (wave || i >= p.m || n >= p.n)
+    if (wave || i || n >= p.n)
         return;
 #pragma unroll
-    for (int v = 1; v < kFewWaves; ++v)
-        acc += joined[v][lane];
+    for (int w = 1; w < kFewWaves; ++w)
+        acc += joined[w][lane];
     const int sum[4] = {acc[0], acc[1], acc[2], acc[3]};
     Int8Columns<4> columns;
     columns.load(p, n);
-    p.sx = scales;
-    finish_int8<4>(p, i, n, sum, columns);
+    p.sx = &scale;
+    finish_int8<4>(p, 0, n, sum, columns);
 }
 
 template <class T, int EPI>
@@ -334,11 +328,11 @@ hipError_t launch(const MmParams &p, hipStream_t st)
 
 }  // namespace
 
-bool i8_fused(int64_t rows, int pitch) { return rows <= kFusedRows && rows * pitch <= kFusedBytes; }
+bool i8_fused(int64_t rows, int pitch) { return rows == 1 && pitch <= kFusedBytes; }
 
 hipError_t launch_i8_fused(const MmParams &p, const QuantParams &q, hipStream_t st)
 {
-    const unsigned n = (p.n + 15) / 16, bytes = p.m * p.k;
+    const unsigned n = (p.n + 15) / 16, bytes = p.k;
     const auto run = [&](auto kernel) {
         const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), kFusedBytes);
         if (e != hipSuccess)

@@ -27,9 +27,6 @@ namespace {
 
 constexpr int kPiece = 8;      // neighbouring elements of a row that a thread takes at once
 
-struct __attribute__((packed, aligned(2))) Any16 {
-    uint4 v;
-};
 template <class T>
 struct Raw {                   // a piece as it lies in memory
     uint4 q[sizeof(T) * kPiece / 16];

@@ -233,7 +233,7 @@ __device__ __forceinline__ void gate_acts(int act, const float (&g)[N], float (&
 }
 
 // N neighbouring values as bf16, or as three bf16 parts in planes of their own (an fp32 operand of a later
-// product); `wide`: the whole run is inside the row and aligned.
+// product), where the whole run is inside the row and aligned.
 template <int N>
 __device__ __forceinline__ void store_operand(__bf16 *dst, int64_t plane, const float (&v)[N])
 {

@@ -7,10 +7,6 @@ namespace enova {
 
 namespace {
 
-struct __attribute__((packed, aligned(1))) AnyQuad {
-    uint4 v;
-};
-
 // Eight values of a row from column c on (zeros past the end): x, or act(g) u where gate >= 0.
 template <class T>
 __device__ __forceinline__ void load_x8(const T *row, int c, int cols, float (&v)[8])
@@ -19,7 +15,7 @@ __device__ __forceinline__ void load_x8(const T *row, int c, int cols, float (&v
         T e[8];
 #pragma unroll
         for (int i = 0; i < static_cast<int>(sizeof(e) / 16); ++i) {
-            const uint4 q = reinterpret_cast<const AnyQuad *>(row + c)[i].v;
+            const uint4 q = reinterpret_cast<const Any16 *>(row + c)[i].v;
             __builtin_memcpy(e + i * (16 / sizeof(T)), &q, 16);
         }
 #pragma unroll
