@@ -41,8 +41,10 @@ typedef struct enova_i8_s *enova_i8;
  * Wd [model][hidden] (contiguous, as torch.nn.Linear stores them).
  * act: SiLU g / (1 + e^-g), GELU g Phi(g) (with erf), or ReLU (derivative 0 at 0).
  * bf16: products of bf16 with fp32 accumulation; h and the gradients of g and u are rounded to bf16
- * once, as operands of the next product, and g and u to 11 bits between the forward and the backward call. f32: operands in three bf16 parts (24 bits),
- * six products; values that are not finite, or past bf16's largest (3.39e38), make NaN of what they reach. */
+ * once, as operands of the next product, and g and u between the forward and the backward call to 11 bits
+ * (and to 2^-39 of the largest of eight neighbours: a smaller one is 0 but for the sign ReLU needs).
+ * f32: operands in three bf16 parts (24 bits, fewer below 2^-110), six products, activations within a few
+ * ulp; values that are not finite, or past bf16's largest (3.39e38), make NaN of what they reach. */
 typedef enum { ENOVA_GATE_SILU = 0, ENOVA_GATE_GELU = 1, ENOVA_GATE_RELU = 2 } enova_gate_act;
 
 typedef struct {
@@ -117,7 +119,8 @@ enova_status enova_resnorm_backward(enova_resnorm op, const void *residual, cons
  *   m = m_scale sign(c) (c / 127)^2, c int8;   sqrt(v) = v_scale (c / 255)^2, c uint8,
  * the scales being the largest |m| and sqrt(v) of the 256. Codes are rounded down after a dither in
  * [0, 1) is added that takes every value evenly over the steps (an average that moves by less than a
- * code's distance each step still moves), and a positive v has a code of 1 at least. */
+ * code's distance each step still moves), and a positive v has a code of 1 at least. Where an m or v of the 256
+ * is not finite, all of them stand for NaN from then on. eps is taken as at least the smallest normal fp32. */
 typedef struct {
     void *param;             /* [numel] */
     const void *grad;        /* [numel] */

@@ -7,7 +7,9 @@ columns next to each other in memory; where a method says so, rows may be furthe
 
 A method that is given a stream works there as torch's own operations do under ``torch.cuda.stream``: what
 it returns is allocated on that stream, and the caller orders the stream after the work that makes the
-arguments, and keeps them until the work is done.
+arguments, and keeps them until the work is done. Calls on one object share its workspace and must not
+overlap: order their streams, or take an object a stream. An object whose calls were captured into a graph
+has to outlive the graph, and a replay counts as such a call.
 """
 from __future__ import annotations
 

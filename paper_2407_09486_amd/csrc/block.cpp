@@ -39,9 +39,9 @@ namespace {
 
 // Up to how many rows a product is taken by the kernels for few rows, whose blocks of 16 weight rows read all of x
 // each: 64 where the tiles would need their operands packed first (fp32: 197 us for 64 rows through 4096 -> 8192,
-// 437 for 65) or where the weights, one matrix's, are less than 8 MiB (8-bit, 1000 -> 8000: 11 us, tiles 14); 16 beyond
-// 16 MiB, from where x's traffic weighs more than a tile's launch (bf16, 4096 -> 8192: 46 us for 16 rows, 57 for 32,
-// 47 by tiles).
+// 437 for 65) or where the weights, one matrix's, are less than 8 MiB (8-bit, 1000 -> 8000: 11 us, tiles 14); 48 from
+// there to 16 MiB, and 16 beyond, where x's traffic weighs more than a tile's launch (bf16, 4096 -> 8192: 46 us for 16
+// rows, 57 for 32, 47 by tiles).
 int few_rows(bool packed, int64_t weight_bytes)
 {
     constexpr int64_t kMiB = int64_t{1} << 20;

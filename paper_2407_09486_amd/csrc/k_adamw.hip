@@ -27,8 +27,8 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// x / d, correctly rounded, for many x of one d: with y the rounded reciprocal of d and q within an ulp of the
-// quotient, q + (x - q d) y rounds to it. `near` says that neither 1 / d nor a quotient of up to 1 leaves the range
+// x / d, correctly rounded, for many x of one d (Markstein's correction): with y the rounded reciprocal of d and q
+// within an ulp of the quotient, q + (x - q d) y rounds to it. `near` says that neither 1 / d nor a quotient of up to 1 leaves the range
 // of normal numbers (a quotient below it is too small to matter to a code); else the plain division is made.
 struct Quotient {
     float d, y;
@@ -44,7 +44,7 @@ struct Quotient {
 };
 
 // The square root of x in [0, 1], correctly rounded but for x too small to matter to a code: the hardware's is
-// within an ulp, and the sign of x - s (s -+ ulp) tells on which side of the half ulp the root is.
+// within an ulp, and the sign of x - s (s -+ ulp) tells on which side of the half ulp the root is (Tuckerman's test).
 __device__ __forceinline__ float unit_sqrt(float x)
 {
     float s = __builtin_amdgcn_sqrtf(x);

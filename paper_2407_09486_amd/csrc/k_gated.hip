@@ -1,12 +1,12 @@
 // Products of the gated feed-forward block (mm_core.h), the finish of those cut into slices, and the bf16
 // operands that products of fp32 or unaligned matrices are made from.
 //
-// An fp32 operand is three bf16 parts, which hold its 24 bits over its whole range, and its product six products of
-// parts, smallest first (a1 b3, a3 b1, a2 b2, a1 b2, a2 b1, a1 b1: what is left out is 2^-26 of it): errors against 64
-// bits are 5e-7 where the fp32 unit's product has 1.4e-6, at 1.2 times its speed (4096 rows, 1024 -> 2048, forward
-// and gradients: 856 us). Two f16 parts under a power of two for each row or column, three products, took 707 us, but
-// hold nothing below 2^-40 of the largest value along the reduction, where a small gradient may meet a large
-// activation: not kept.
+// An fp32 operand is three bf16 parts, which hold its 24 bits from 2^-110 up (below, the third ends under bf16's
+// smallest number), and its product six products of parts, smallest first (a1 b3, a3 b1, a2 b2, a1 b2, a2 b1, a1 b1: what
+// is left out is 2^-26 of it): errors against 64 bits are 5e-7 where the fp32 unit's product has 1.5e-6, at 1.3 times its
+// rate (4096 rows, 1024 -> 2048, forward and gradients: 869 us). Two f16 parts under a power of two for each row or
+// column, three products, took 707 us, but hold nothing below 2^-40 of the largest value along the reduction, where a
+// small gradient may meet a large activation: not kept.
 #include <algorithm>
 
 #include "mm_core.h"

@@ -20,6 +20,8 @@
 // eight waves of 128 x 64 outputs (a 256-tile): four waves of 128 x 128 read a third less LDS, but have nothing to run
 // while one waits (915 us). Fragments are read half a slab ahead of their use, and reads and loads are spread between the
 // operations (all at once, after the barrier: 994 us). A 128-tile, two to a compute unit, serves smaller products.
+// The 256-tile's 128 sums and two sets of fragments leave few of a thread's 256 registers: of its instances the one for
+// two operands in columns keeps 52 bytes a thread in scratch memory, and the gate's for ragged reductions 20.
 //
 // The loads to LDS are written out as instructions: the compiler, which cannot tell the two buffers apart,
 // waits for every load to LDS before the next LDS read. They write no register, and every wave waits for its
