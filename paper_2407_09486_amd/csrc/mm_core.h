@@ -181,7 +181,7 @@ struct Fragments {
 };
 
 // act(g) and its derivative. EXACT (blocks of fp32): within a few ulp of the result, GELU with expf and erfcf. Else (bf16,
-// whose next rounding is 2^-9, and 8-bit codes) the hardware's exponential and reciprocal, an ulp each, the former of a
+// whose next rounding is up to 2^-8, and 8-bit codes) the hardware's exponential and reciprocal, an ulp each, the former of a
 // rounded product (a relative |g| 2^-24 more), and for GELU Phi from Abramowitz and Stegun's formula 7.1.26 for erf,
 // sharing the exponential with the density: within 2.5e-7, which is no more than the order of the tail where g < -5.
 // With expf, erff and division a tile of the bf16 hidden gradient spent as long on them as on memory

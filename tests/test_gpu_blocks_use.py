@@ -6,7 +6,8 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from paper_2407_09486_amd import binding  # noqa: E402
-from test_gpu_blocks import block64, block_inputs, blocks, close, norm_inputs, normal, rng, run_block, run_norm  # noqa: E402
+from test_gpu_blocks import (act64, adam64, adam_inputs, block64, block_inputs, blocks, close, norm_inputs, normal, rng,  # noqa: E402
+                             run_block, run_norm)
 
 
 # ----------------------------------------------------------------------------- graphs
@@ -295,3 +296,47 @@ def test_adamw_states_into_one_list_given():
         got = op.states(**{"mv"[which]: mine})
         assert all(a is b for a, b in zip(got[which], mine))
         assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("rows", [20, 90])
+@pytest.mark.parametrize("act", ["gelu", "relu"])
+def test_block_f32_rows_of_all_sizes_with_other_activations(act, rows):
+    """As for SiLU in test_gpu_blocks_edges.py: within four times the worst row of the formula in fp32."""
+    t = block_inputs(rows, 72, 136, "f32", 21)
+    size = 10.0 ** torch.linspace(-8, 8, rows, device="cuda")[:, None]
+    t[0] *= size
+    t[4] /= size
+    t[4][:, 5] *= 1e-6
+    t[3][:, 9] *= 1e-6
+    got = run_block(blocks.GatedBlock(72, 136, dtype="f32", act=act), *t)
+    v = [a.cpu().requires_grad_(True) for a in t[:4]]
+    y = (act64(v[0] @ v[1].T, act) * (v[0] @ v[2].T)) @ v[3].T
+    plain = [y.detach(), *torch.autograd.grad(y, v, t[4].cpu())]
+
+    def worst(a, b):
+        return float(((a.double().cpu() - b).norm(dim=1) / b.norm(dim=1)).max())
+
+    for name, a, f, b in zip(("y", "dx", "dwg", "dwu", "dwd"), got, plain, block64(*t, act)):
+        assert worst(a, b) <= 4 * worst(f, b), (name, worst(a, b), worst(f, b))
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+def test_adamw_bf16_parameters_with_8_bit_states(grad, shift):
+    """A step from the states' own values: p is the rounding of the formula's, m and sqrt(v) within a code and its dither."""
+    p, g = adam_inputs("bf16", grad, 6, shift)
+    op = blocks.AdamW(p, g, bits=8, lr=1e-2)
+    m, v = ([a.clone() for a in s] for s in op.states())
+    for n in range(1, 5):
+        before = [a.double() for a in p]
+        op.step(grad_scale=2.0)
+        got_m, got_v = op.states()
+        for i in range(len(p)):
+            q, wm, wv = adam64(before[i], 2.0 * g[i].double(), m[i].double(), v[i].double(), n, 1e-2)
+            off = 3e-7 * q.abs() + 1e-7        # three roundings in fp32, and ten of an update of up to 0.1
+            assert ((p[i] >= (q - off).bfloat16()) & (p[i] <= (q + off).bfloat16())).all()
+            for part in range(0, p[i].numel(), 256):
+                s = slice(part, part + 256)
+                assert (got_m[i][s] - wm[s]).abs().max() <= wm[s].abs().max() * (2 / 127) + 1e-12
+                assert (got_v[i][s].double().sqrt() - wv[s].sqrt()).abs().max() <= wv[s].sqrt().max() * (2 / 255) + 1e-12
+        m, v = ([a.clone() for a in s] for s in (got_m, got_v))
